@@ -181,7 +181,8 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
       inv_total = (float)scale;
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = x[r] == -__builtin_inff() ? kNone : key_of(key[r] * scale + (double)given[r], e0 + r);
+    for (int r = 0; r < R; ++r)            // (closed by either, whatever the score is: a NaN plus -inf is a NaN)
+      key[r] = x[r] == -__builtin_inff() || given[r] == -__builtin_inff() ? kNone : key_of(key[r] * scale + (double)given[r], e0 + r);
   }
   if (a.groups > 1) keep_groups<L, R>(a, key, l, (in_lds<double>*)group_keys + (threadIdx.x / L) * a.experts);
 

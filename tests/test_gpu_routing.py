@@ -207,3 +207,42 @@ def test_route_gradient_against_differences_of_the_forward(hap):
                         continue                                            # the step changes the choice
                     num = ((wu - wl)[t] * g[t]).sum() / (2 * step)
                     assert abs(num - host(dx)[t, e]) <= np.abs(g[t]).sum() * (step ** 2 + 60 * U / step)
+
+
+def routed(hap, x, k, sigmoid, renorm, bias=None, groups=1, top=None, best=1, dw=None, scale=1.0):
+    """fp32 logits through both entry points: (indices, weights, dlogits) as numpy."""
+    torch = torch_mod()
+    T, E = x.shape
+    xd = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda()
+    bd = torch.from_numpy(np.asarray(bias, dtype=np.float32)).cuda() if bias is not None else None
+    desc = hap.RouteDesc(T, E, k, hap.F32, score=int(sigmoid), groups=groups, top_groups=top, group_best=best, renormalise=renorm, scale=scale)
+    idx = torch.full((T, k), -7, dtype=torch.int32, device="cuda"); w = torch.full((T, k), -7.0, device="cuda"); dx = torch.full((T, E), -7.0, device="cuda")
+    hap.hap_moe_route_fwd(desc, xd, bd, idx, w)
+    g = torch.ones((T, k), device="cuda") if dw is None else torch.from_numpy(dw.astype(np.float32)).cuda()
+    hap.hap_moe_route_bwd(desc, xd, idx, g, dx)
+    return idx.cpu().numpy(), host(w), host(dx)
+
+
+@pytest.mark.parametrize("sigmoid,renorm", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("E,groups,best", [(8, 1, 1), (30, 1, 1), (30, 5, 2), (64, 8, 2), (256, 8, 1), (320, 10, 2), (700, 1, 1)])
+def test_route_barred_experts_are_never_chosen(hap, sigmoid, renorm, E, groups, best):
+    """A bias (or a logit) of -inf closes an expert whatever its score is: NaN in its own column, NaN or +inf in others."""
+    rng = np.random.default_rng(E + groups)
+    x = rng.normal(size=(7, E)).astype(np.float32)
+    barred = np.arange(E) % 5 == 2
+    bias = np.where(barred, -np.inf, rng.normal(size=E) * 0.2)
+    x[1, 2] = np.nan                                          # one barred column
+    x[2, barred] = np.nan                                     # all of them
+    x[3, 2] = np.inf
+    x[4, 5] = np.nan                                          # an open one
+    x[5, :] = np.nan
+    x[6, 2] = np.nan; x[6, 3:] = -np.inf
+    k = 4
+    idx, w, _ = routed(hap, x, k, sigmoid, renorm, bias, groups, None, best)
+    assert ((idx >= -1) & (idx < E)).all() and not barred[idx[idx >= 0]].any(), idx
+    assert all(len(set(r[r >= 0])) == (r >= 0).sum() for r in idx) and (w[idx < 0] == 0).all()
+    assert set(idx[6]) == {0, 1, -1}
+    shut = np.where(barred, -np.inf, x)                       # sigmoid scores of the others do not depend on the barred columns
+    rows = [0, 1, 2, 3, 6] if sigmoid else [0]
+    oi, ow = ort.route_fwd((shut if sigmoid else x)[rows].astype(np.float64), k, sigmoid, bias.astype(np.float32).astype(np.float64), groups, None, best, renorm)
+    assert (idx[rows] == oi).all() and (np.abs(w[rows] - ow) <= (40 + 2 * np.abs(x[0]).max()) * U * np.abs(ow)).all()
