@@ -418,7 +418,7 @@ int hap_reducescatter_split(const hap_gather_desc* d, const void* full, int64_t 
  *     weight of a chosen expert: scale * s, with renormalise scale * s / (sum of s over the chosen)
  * An expert whose logit or bias is -inf is never chosen; a choice that finds no expert has index -1 and weight 0 (a token all of whose
  * logits are -inf goes nowhere).  The order is that of the scores before rounding: without a bias the logits' own order, exactly;
- * scores plus bias, and sums over groups, are formed in fp64 and compared to 42 bits.  NaN ranks
+ * scores plus bias, and sums over groups, are formed and compared in fp64.  NaN ranks
  * above every number; a NaN among the logits (or +inf under softmax) makes the token's weights NaN, its indices stay valid.
  * tokens < 2^26, experts <= 1024, top_k <= 64, groups <= 64 (HAP_EUNSUPPORTED beyond); groups divides experts; top_k <= top_groups * experts / groups. */
 typedef enum { HAP_SCORE_SOFTMAX = 0, HAP_SCORE_SIGMOID = 1 } hap_score;

@@ -87,6 +87,12 @@ __device__ __forceinline__ int sum_up_to_lane(int v) {
   return v;
 }
 
+/* The lowest of the L lanes around this one (counted from their first) whose bit is set in a ballot; one of them is. */
+template <int L> __device__ __forceinline__ int lowest_lane(uint64_t ballot) {
+  if constexpr (L == 64) return __builtin_ctzll(ballot);
+  else return __builtin_ctz(((threadIdx.x & 32) ? (uint32_t)(ballot >> 32) : (uint32_t)ballot) >> (threadIdx.x & 31 & ~(unsigned)(L - 1)));
+}
+
 /* Lane i's value, i the same in all lanes. */
 __device__ __forceinline__ uint32_t from_lane(uint32_t v, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)v, i); }
 __device__ __forceinline__ int from_lane(int v, int i) { return __builtin_amdgcn_readlane(v, i); }

@@ -6,7 +6,7 @@
  *   that stay;  w_i = scale * s[e_i], divided by the sum over the chosen where asked
  *
  * The choice follows the scores before any rounding.  Without a bias both scores rise with the logit, so the logits themselves are compared,
- * exactly; where sums decide (a bias, the best two of a group) they are formed in fp64, and compared to 42 bits.
+ * exactly; where sums decide (a bias, the best two of a group) they are formed and compared in fp64.
  */
 #include <hip/hip_runtime.h>
 
@@ -60,37 +60,41 @@ template <typename T, int R, bool INTERLEAVED> __device__ __forceinline__ void l
   }
 }
 
-/* ---- keys: a number with the index of what it belongs to in its last ten bits, as a double.  The greater key wins, equal numbers go by the lower index: one
- * v_max_f64 decides both and carries the index along.  fp32 numbers are exact (29 of a double's bits are free), fp64 sums keep 42 bits.  NaN ranks above
- * everything; kNone (and anything as low, which no fp32 number or sum of them is) stands for what cannot be chosen. */
-constexpr double kNone = -1.7e308;
-__device__ __forceinline__ double key_of(double v, int index) {
-  if (v == -__builtin_inf()) return kNone;
-  v = v != v ? 0x1.fffffffffff00p+1023 : fmin(v, 0x1.ffffffffff800p+1023) + 0.0;      // (-0 is 0)
-  const uint64_t b = (uint64_t)__double_as_longlong(v);
+/* ---- ranks: numbers as they are compared, NaN above everything and the infinities as finite ones in their order (v_max_f64 passes a NaN over); kNone (and anything
+ * as low, which no fp32 number or sum of them is) stands for what cannot be chosen. */
+constexpr double kNone = -1.7e308, kInfinite = 0x1.ffffffffff800p+1023, kNan = 0x1.fffffffffff00p+1023;
+__device__ __forceinline__ double rank_of(double v) {
+  const double low = fmax(fmin(v, kInfinite), kNone);                 // (of a NaN: either bound)
+  return v != v ? kNan : low;
+}
+__device__ __forceinline__ bool is_rank(double k) { return k > -1e300; }
+template <int L> __device__ __forceinline__ double greatest(double k) { return fold<L>(k, [](double a, double b) { return fmax(a, b); }); }
+
+/* ---- keys: the rank of an fp32 number with the index of what it belongs to in its last ten bits (29 of a double's are free).  The greater key wins, equal numbers go by
+ * the lower index: one v_max_f64 decides both and carries the index along. */
+__device__ __forceinline__ double key_of(double rank, int index) {
+  if (rank == kNone) return kNone;
+  const uint64_t b = (uint64_t)__double_as_longlong(rank + 0.0);      // (-0 is 0)
   return __longlong_as_double((long long)((b & ~(uint64_t)1023) | (uint64_t)((b >> 63) ? index : 1023 - index)));
 }
-__device__ __forceinline__ bool is_key(double k) { return k > -1e300; }
 __device__ __forceinline__ int index_of(double k) {
   const uint64_t b = (uint64_t)__double_as_longlong(k);
   const int low = (int)(b & 1023);
   return (b >> 63) ? low : 1023 - low;
 }
-__device__ __forceinline__ double number_of(double k) { return __longlong_as_double((long long)((uint64_t)__double_as_longlong(k) & ~(uint64_t)1023)); }
-template <int L> __device__ __forceinline__ double greatest(double k) { return fold<L>(k, [](double a, double b) { return fmax(a, b); }); }
 
-/* The two greatest keys of a set. */
+/* The two greatest of a set. */
 struct Two { double first, second; };
 __device__ __forceinline__ Two merge(Two a, Two b) { return {fmax(a.first, b.first), fmax(fmin(a.first, b.first), fmax(a.second, b.second))}; }
 
-/* Closes (kNone) the keys of all groups but the top_groups best.  `scratch`: LDS for the token's keys, where groups are no whole lanes. */
-template <int L, int R> __device__ __forceinline__ void keep_groups(const RouteArgs& a, double (&key)[R], int l, volatile in_lds<double>* scratch) {
+/* Closes (kNone) the ranks of all groups but the top_groups best.  `scratch`: LDS for the token's ranks, where groups are no whole lanes. */
+template <int L, int R> __device__ __forceinline__ void keep_groups(const RouteArgs& a, double (&rank)[R], int l, volatile in_lds<double>* scratch) {
   const int e0 = l * R, span = a.group_lanes;
   Two two = {kNone, kNone};
   if (span) {
     // a group is `span` whole lanes: its best two by a butterfly over them, in every lane of it
 #pragma unroll
-    for (int r = 0; r < R; ++r) two = merge(two, Two{key[r], kNone});
+    for (int r = 0; r < R; ++r) two = merge(two, Two{rank[r], kNone});
     if (span > 1) two = merge(two, Two{partner<1>(two.first), partner<1>(two.second)});
     if constexpr (L > 2) if (span > 2) two = merge(two, Two{partner<2>(two.first), partner<2>(two.second)});
     if constexpr (L > 4) if (span > 4) two = merge(two, Two{partner<4>(two.first), partner<4>(two.second)});
@@ -100,39 +104,44 @@ template <int L, int R> __device__ __forceinline__ void keep_groups(const RouteA
     // (one wave: its LDS operations keep their order)
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if (e0 + r < a.experts) scratch[e0 + r] = key[r];
+      if (e0 + r < a.experts) scratch[e0 + r] = rank[r];
     __builtin_amdgcn_wave_barrier();
     if (l < a.groups)                  // (as many lanes as groups: the host chose L)
       for (int e = 0; e < a.per_group; ++e) two = merge(two, Two{scratch[l * a.per_group + e], kNone});
     __builtin_amdgcn_wave_barrier();
   }
-  const int group = span ? l / span : l;
-  double score = !is_key(two.first) ? kNone : key_of(a.best > 1 && is_key(two.second) ? number_of(two.first) + number_of(two.second) : number_of(two.first), group);
-  uint64_t stays = 0;
+  // the best group is that of the lowest lane that has the greatest sum
+  double score = a.best > 1 && is_rank(two.second) ? (two.first == kNan ? kNan : fmin(two.first + two.second, kInfinite)) : two.first;
+  const int unit = span ? span : 1;
+  uint64_t stays = 0;                  // lanes of the groups that stay, each group's lowest
+  bool mine = false;
   for (int i = 0; i < a.top_groups; ++i) {
-    const double k = greatest<L>(score);
-    if (!is_key(k)) break;
-    const int g = index_of(k);
-    stays |= 1ull << g;
-    if (g == group) score = kNone;
+    const double best = greatest<L>(score);
+    if (!is_rank(best)) break;
+    const int won = lowest_lane<L>(__ballot(score == best));
+    stays |= 1ull << won;
+    if (((won ^ l) & -unit) == 0) { mine = true; score = kNone; }
   }
+  if (span) {
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int g = span ? group : e0 + r < a.experts ? (e0 + r) / a.per_group : 0;
-    if (!((stays >> g) & 1)) key[r] = kNone;
+    for (int r = 0; r < R; ++r) rank[r] = mine ? rank[r] : kNone;
+  } else {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (e0 + r < a.experts && !((stays >> ((e0 + r) / a.per_group)) & 1)) rank[r] = kNone;
   }
 }
 
-/* One token per L lanes, R consecutive experts per lane; choice i of the token ends up in lane i.  SUMS: biases or sums of scores decide; otherwise the
- * logits themselves are the keys.
+/* One token per L lanes, R consecutive experts per lane; choice i of the token ends up in lane i.  SUMS: biases or sums of scores decide, formed and compared in fp64;
+ * otherwise the logits themselves, as keys.
  *
- * Bound: instructions (the logits are a few MB).  A choice is a maximum over the lane's own keys and a butterfly, both of v_max_f64; few lanes with many
- * experts each do more tokens per instruction than one lane per expert.  8192 tokens, 8 of 256 in groups: 30 us with one token per wave, integer keys and
- * indices exchanged beside them, 15.5 with four tokens per wave, 11.6 with these keys, 21 with sums in fp32 that fall back to fp64 where they do not decide (the few waves that
- * do set the time). */
+ * Bound: instructions (the logits are a few MB).  A choice is a maximum over the lane's own ranks and a butterfly, both of v_max_f64; few lanes with many
+ * experts each do more tokens per instruction than one lane per expert.  8192 tokens, 8 of 256 in groups, bias and sums: 30 us with one token per wave, integer keys
+ * and indices exchanged beside them, 21 with sums in fp32 that fall back to fp64 where they do not decide (the few waves that do set the time), 11.8 now.  Keys
+ * decide the logits' order (7.5 us for the same without sums); for sums they would leave 42 bits to compare (11.4 us, and sigmoid scores of logits above 30 equal). */
 template <typename T, int L, int R, bool SUMS>
 __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const T* logits, const float* bias, int* indices, float* weights) {
-  extern __shared__ double group_keys[];            // [tokens of the block][experts], where groups are no whole lanes
+  extern __shared__ double group_ranks[];           // [tokens of the block][experts], where groups are no whole lanes
   const int l = threadIdx.x % L, e0 = l * R;
   int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
   const bool live = t < a.tokens;
@@ -158,7 +167,7 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
     top = fold<L>(top, [](float p, float q) { return fmaxf(p, q); });
     if (top == -__builtin_inff()) top = 0.0f;       // nothing can be chosen: no score is needed
   }
-  double key[R];
+  double rank[R];
   if constexpr (!SUMS) {
     if (!a.sigmoid && !a.renormalise) {
       float s = 0.0f;
@@ -167,40 +176,65 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
       inv_total = 1.0f / sum<L>(s);
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) key[r] = key_of((double)x[r], e0 + r);
+    for (int r = 0; r < R; ++r) rank[r] = rank_of((double)x[r]);
   } else {
     double scale = 1.0;
     if (a.sigmoid) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) key[r] = 1.0 / (1.0 + exp(-(double)x[r]));
+      for (int r = 0; r < R; ++r) rank[r] = 1.0 / (1.0 + exp(-(double)x[r]));
     } else {
       double n = 0.0;
 #pragma unroll
-      for (int r = 0; r < R; ++r) { key[r] = exp((double)x[r] - (double)top); n += key[r]; }
+      for (int r = 0; r < R; ++r) { rank[r] = exp((double)x[r] - (double)top); n += rank[r]; }
       scale = 1.0 / sum<L>(n);
       inv_total = (float)scale;
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r)            // (closed by either, whatever the score is: a NaN plus -inf is a NaN)
-      key[r] = x[r] == -__builtin_inff() || given[r] == -__builtin_inff() ? kNone : key_of(key[r] * scale + (double)given[r], e0 + r);
+    for (int r = 0; r < R; ++r) {          // (closed by either, whatever the score is: a NaN plus -inf is a NaN)
+      const bool shut = (x[r] == -__builtin_inff()) | (given[r] == -__builtin_inff());
+      const double c = rank_of(rank[r] * scale + (double)given[r]);
+      rank[r] = shut ? kNone : c;
+    }
   }
-  if (a.groups > 1) keep_groups<L, R>(a, key, l, (in_lds<double>*)group_keys + (threadIdx.x / L) * a.experts);
+  if (a.groups > 1) keep_groups<L, R>(a, rank, l, (in_lds<double>*)group_ranks + (threadIdx.x / L) * a.experts);
 
+  if constexpr (!SUMS) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) rank[r] = key_of(rank[r], e0 + r);
+  }
   int chosen = -1;
   for (int i = 0; i < a.top_k; ++i) {
     double k[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) k[r] = key[r];
+    for (int r = 0; r < R; ++r) k[r] = rank[r];
 #pragma unroll
     for (int n = R / 2; n > 0; n /= 2)
 #pragma unroll
       for (int r = 0; r < n; ++r) k[r] = fmax(k[r], k[r + n]);
     const double best = greatest<L>(k[0]);
-    if (!is_key(best)) break;
-    if (l == i) chosen = index_of(best);
+    if (!is_rank(best)) break;
+    const auto close = [&](int r, bool taken) {      // (one word: below every number)
+      rank[r] = __hiloint2double(taken ? (int)0xffe00000 : __double2hiint(rank[r]), __double2loint(rank[r]));
+    };
+    if constexpr (!SUMS) {
+      if (l == i) chosen = index_of(best);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      key[r] = __hiloint2double(key[r] == best ? (int)0xffe00000 : __double2hiint(key[r]), __double2loint(key[r]));      // (one word: below every number)
+      for (int r = 0; r < R; ++r) close(r, rank[r] == best);
+    } else {
+      // all 64 bits are compared: of equals the lowest lane's first
+      const int won = lowest_lane<L>(__ballot(k[0] == best));
+      bool open = l == won;
+      int e = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const bool taken = open & (rank[r] == best);
+        e = taken ? e0 + r : e;
+        close(r, taken);
+        open = open & !taken;
+      }
+      e = __shfl(e, won, L);
+      if (l == i) chosen = e;
+    }
   }
 
   const float xi = chosen >= 0 ? to_f32(row[chosen]) : -__builtin_inff();

@@ -246,3 +246,44 @@ def test_route_barred_experts_are_never_chosen(hap, sigmoid, renorm, E, groups, 
     rows = [0, 1, 2, 3, 6] if sigmoid else [0]
     oi, ow = ort.route_fwd((shut if sigmoid else x)[rows].astype(np.float64), k, sigmoid, bias.astype(np.float32).astype(np.float64), groups, None, best, renorm)
     assert (idx[rows] == oi).all() and (np.abs(w[rows] - ow) <= (40 + 2 * np.abs(x[0]).max()) * U * np.abs(ow)).all()
+
+
+def test_route_group_sums_are_formed_before_anything_is_cut(hap):
+    """Groups whose best two all but cancel, -1/2 and 1/2, 1/2 + 2^-46 or 1/2 + 2^-45: exact sums of exact 64-bit scores, which 42 bits of each score do not tell apart."""
+    for per in (2, 3, 8, 20):                                 # groups inside a lane, across lanes, no whole lanes
+        E = 3 * per
+        x = np.zeros((2, E))
+        x[1, per:] = -np.inf; x[1, 0:2] = 0; x[1, per:per + 2] = 0; x[1, 2 * per:2 * per + 2] = 0
+        bias = np.full(E, -2.0)
+        bias[0], bias[1] = 0.0, -1.0                          # 0
+        bias[per], bias[per + 1] = 2.0 ** -46, -1.0           # 2^-46
+        bias[2 * per], bias[2 * per + 1] = 2.0 ** -45, -1.0   # 2^-45
+        got = run_route(hap, x, "f32", 2, True, True, bias=bias, groups=3, top=1, best=2)
+        assert (got == [[2 * per, 2 * per + 1]] * 2).all(), (per, got)
+        got = run_route(hap, x, "f32", 4, True, True, bias=bias, groups=3, top=2, best=2)
+        assert all(set(r // per) == {1, 2} for r in got), (per, got)
+
+
+def test_route_groups_with_infinite_biases_and_nan(hap):
+    """A group that holds a NaN comes before one whose sum is +inf, that before numbers."""
+    x = np.zeros((3, 24), dtype=np.float32)
+    bias = np.zeros(24); bias[[4, 5]] = np.inf; bias[9] = np.inf
+    x[1, 20] = np.nan
+    x[2, [20, 21]] = np.nan
+    for best in (1, 2):
+        idx, _, _ = routed(hap, x, 2, True, False, bias, 6, 1, best)
+        assert idx[0].tolist() == [4, 5] and set(idx[1]) == {20, 21} and set(idx[2]) == {20, 21} and idx[1, 0] == 20
+        idx, _, _ = routed(hap, x, 3, True, False, bias, 6, 2, best)
+        assert idx[0].tolist() == [4, 5, 9] and idx[1].tolist() == [20, 4, 5] and set(idx[2]) == {20, 21, 4}
+
+
+def test_route_scores_with_a_bias_are_compared_in_64_bits(hap):
+    """Sigmoids of 28 to 34, which agree to 40 bits and more, below a bias that moves some of them by 2^-44."""
+    rng = np.random.default_rng(12)
+    for E, groups in ((16, 1), (30, 1), (64, 4), (256, 8), (512, 1), (900, 1)):
+        x = rng.integers(-3, 4, size=(6, E)).astype(np.float64)
+        for t in range(6):
+            x[t, rng.permutation(E)[:7]] = rng.permutation(7) + 28.0
+        bias = np.zeros(E); bias[rng.random(E) < 0.2] = 2.0 ** -44
+        for best in (1, 2):
+            run_route(hap, x, "f32", 7, True, True, bias=bias, groups=groups, best=best, seed=E)
