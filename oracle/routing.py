@@ -4,7 +4,7 @@
     stay, descending, equals by the lower index;  weight = scale * s, divided by the sum over the chosen where asked
 
 An expert whose logit or bias is -inf is never chosen; a choice that finds none is -1 with weight 0.  Without a bias the logits' order is the
-scores' order.  Everything is computed token by token, in float64.
+scores' order, also inside groups that rank by sums of scores.  Everything is computed token by token, in float64.
 
     plan      choice n = t * k + i takes the row of its expert's buffer that counts the choices before it; -1 beyond the capacity
     dispatch  X_e[position] = x[t];   combine  out[t] = sum_i w_i Y_e[position]
@@ -44,6 +44,8 @@ def choose(x, top_k, sigmoid=False, bias=None, groups=1, top_groups=None, group_
             score.append(sum(members[:group_best]) if members else None)
         ranked = sorted((g for g in range(groups) if score[g] is not None), key=lambda g: (-score[g], g))[:top_groups]
         open_ = [open_[e] and e // per in ranked for e in range(E)]
+    if bias is None:
+        c = [float(v) for v in x]                 # (what the groups' sums were taken of ranks groups only)
     order = sorted((e for e in range(E) if open_[e]), key=lambda e: (-c[e], e))[:top_k]
     return order + [-1] * (top_k - len(order))
 

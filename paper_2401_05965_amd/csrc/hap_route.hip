@@ -6,7 +6,7 @@
  *   that stay;  w_i = scale * s[e_i], divided by the sum over the chosen where asked
  *
  * The choice follows the scores before any rounding.  Without a bias both scores rise with the logit, so the logits themselves are compared,
- * exactly; where sums decide (a bias, the best two of a group) they are formed and compared in fp64.
+ * exactly; where sums decide (scores with a bias; among groups also the best two of each) they are formed and compared in fp64.
  */
 #include <hip/hip_runtime.h>
 
@@ -132,30 +132,31 @@ template <int L, int R> __device__ __forceinline__ void keep_groups(const RouteA
   }
 }
 
-/* One token per L lanes, R consecutive experts per lane; choice i of the token ends up in lane i.  SUMS: biases or sums of scores decide, formed and compared in fp64;
- * otherwise the logits themselves, as keys.
+enum Order { kLogits, kSumsOfGroups, kSums };      // what is compared
+
+/* One token per L lanes, R consecutive experts per lane; choice i of the token ends up in lane i.  kSums: scores with a bias decide, formed and compared in fp64;
+ * otherwise the logits themselves, as keys, in groups that rank by their best logit or (kSumsOfGroups) by sums of scores.
  *
  * Bound: instructions (the logits are a few MB).  A choice is a maximum over the lane's own ranks and a butterfly, both of v_max_f64; few lanes with many
  * experts each do more tokens per instruction than one lane per expert.  8192 tokens, 8 of 256 in groups, bias and sums: 30 us with one token per wave, integer keys
  * and indices exchanged beside them, 21 with sums in fp32 that fall back to fp64 where they do not decide (the few waves that do set the time), 11.8 now.  Keys
  * decide the logits' order (7.5 us for the same without sums); for sums they would leave 42 bits to compare (11.4 us, and sigmoid scores of logits above 30 equal). */
-template <typename T, int L, int R, bool SUMS>
+template <typename T, int L, int R, Order ORDER>
 __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const T* logits, const float* bias, int* indices, float* weights) {
+  constexpr bool SUMS = ORDER != kLogits, KEYS = ORDER != kSums;
   extern __shared__ double group_ranks[];           // [tokens of the block][experts], where groups are no whole lanes
   const int l = threadIdx.x % L, e0 = l * R;
   int64_t t = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
   const bool live = t < a.tokens;
   if (!live) t = a.tokens - 1;
   const T* row = logits + t * a.ld;
-  float x[R], given[SUMS ? R : 1];
+  float x[R], given[R];
   load_values<T, R, false>(row, l, L, a.experts, a.vec, -__builtin_inff(), x);
-  if constexpr (SUMS) {
-    if (bias) {
-      load_values<float, R, false>(bias, l, L, a.experts, a.vec_bias, 0.0f, given);
-    } else {
+  if constexpr (ORDER == kSums) {
+    load_values<float, R, false>(bias, l, L, a.experts, a.vec_bias, 0.0f, given);
+  } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r) given[r] = 0.0f;
-    }
+    for (int r = 0; r < R; ++r) given[r] = 0.0f;
   }
 
   // statistics of the whole row, where the scores are a softmax over all of it
@@ -198,9 +199,12 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
   }
   if (a.groups > 1) keep_groups<L, R>(a, rank, l, (in_lds<double>*)group_ranks + (threadIdx.x / L) * a.experts);
 
-  if constexpr (!SUMS) {
+  if constexpr (KEYS) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) rank[r] = key_of(rank[r], e0 + r);
+    for (int r = 0; r < R; ++r) {          // (the sums were the groups': inside them the logits decide, whose scores may be equal)
+      const double logit = rank_of((double)x[r]);
+      rank[r] = key_of(!SUMS ? rank[r] : is_rank(rank[r]) ? logit : kNone, e0 + r);
+    }
   }
   int chosen = -1;
   for (int i = 0; i < a.top_k; ++i) {
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
     const auto close = [&](int r, bool taken) {      // (one word: below every number)
       rank[r] = __hiloint2double(taken ? (int)0xffe00000 : __double2hiint(rank[r]), __double2loint(rank[r]));
     };
-    if constexpr (!SUMS) {
+    if constexpr (KEYS) {
       if (l == i) chosen = index_of(best);
 #pragma unroll
       for (int r = 0; r < R; ++r) close(r, rank[r] == best);
@@ -384,12 +388,13 @@ template <typename T> int route_fwd_t(RouteArgs a, const void* logits, const flo
   with_layout(a, [&](auto l, auto r) {
     constexpr int L = decltype(l)::value, R = decltype(r)::value;
     const dim3 grid((unsigned)((a.tokens + 256 / L - 1) / (256 / L)));
-    const bool wide = bias || (a.groups > 1 && a.best > 1);
     const int gl = a.per_group % R ? 0 : a.per_group / R;
     a.group_lanes = gl && (gl & (gl - 1)) == 0 && gl < L ? gl : 0;
     const size_t lds = a.groups > 1 && !a.group_lanes ? (size_t)(256 / L) * a.experts * 8 : 0;
-    if (wide) hipLaunchKernelGGL((route_fwd_kernel<T, L, R, true>), grid, dim3(256), lds, s, a, (const T*)logits, bias, indices, weights);
-    else hipLaunchKernelGGL((route_fwd_kernel<T, L, R, false>), grid, dim3(256), lds, s, a, (const T*)logits, bias, indices, weights);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a, (const T*)logits, bias, indices, weights); };
+    if (bias) launch(route_fwd_kernel<T, L, R, kSums>);
+    else if (a.groups > 1 && a.best > 1) launch(route_fwd_kernel<T, L, R, kSumsOfGroups>);
+    else launch(route_fwd_kernel<T, L, R, kLogits>);
   });
   return check_launch("moe_route_fwd");
 }

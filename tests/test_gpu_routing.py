@@ -287,3 +287,37 @@ def test_route_scores_with_a_bias_are_compared_in_64_bits(hap):
         bias = np.zeros(E); bias[rng.random(E) < 0.2] = 2.0 ** -44
         for best in (1, 2):
             run_route(hap, x, "f32", 7, True, True, bias=bias, groups=groups, best=best, seed=E)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_route_order_inside_groups_is_that_of_the_logits_without_a_bias(hap, sigmoid, renorm):
+    """Groups by the sums of their best two scores, the choice inside them by the logits: scores that are equal to 42 bits (sigmoids of 30 and more), in 64 bits (of 38 and
+    more; softmax scores 800 below the row's largest) and logits one fp32 step apart."""
+    step = lambda v, n: float(np.nextafter(np.float32(v), np.float32(np.inf))) if n == 1 else step(step(v, 1), n - 1)
+    x = np.full((4, 16), -3.0)
+    x[0, [1, 2, 3]] = [30.0, 33.0, 31.0]; x[0, [8, 9]] = [29.0, 35.0]
+    x[1, [0, 1, 2]] = [60.0, step(60.0, 1), step(60.0, 2)]; x[1, [12, 13]] = [45.0, 44.0]
+    x[2, :] = -900.0; x[2, 5] = 10.0; x[2, [1, 9]] = [-899.0, -898.0]
+    x[3, [4, 5, 6, 7]] = [1.0, step(1.0, 1), step(1.0, 2), step(1.0, 3)]
+    for groups in (2, 4, 8):                                   # whole lanes and parts of a lane
+        got = run_route(hap, x, "f32", 5, sigmoid, renorm, groups=groups, best=2)
+        assert got[0].tolist() == [9, 2, 3, 1, 8] and got[1].tolist()[:5] == [2, 1, 0, 12, 13]
+        assert got[2].tolist()[:3] == [5, 9, 1] and got[3].tolist()[:4] == [7, 6, 5, 4]
+    # three groups of four are kept, the one without large logits is not
+    y = np.full((2, 16), -5.0)
+    y[0, [1, 2, 4, 5, 13, 14]] = [31.0, 35.0, 34.0, 33.0, 32.0, 30.0]
+    y[1, [3, 0, 8, 11, 12, 15]] = [3.0, 3.0, 2.0, 4.0, 1.0, 5.0]
+    got = run_route(hap, y, "f32", 6, sigmoid, renorm, groups=4, top=3, best=2)
+    assert got[0].tolist() == [2, 4, 5, 13, 1, 14] and got[1].tolist() == [15, 11, 0, 3, 8, 12]
+
+
+@pytest.mark.parametrize("E", [40, 96, 320, 512, 1024])
+def test_route_order_inside_groups_over_layouts(hap, E):
+    """Far and near logits, every group kept, so that only the choice's order counts."""
+    rng = np.random.default_rng(E)
+    x = rng.normal(size=(9, E)) * 40
+    x[::2] = np.round(x[::2])                                 # equals among them
+    for groups in (2, E // 4, 8) if E < 200 else (2, 8, 32):
+        for sigmoid in (False, True):
+            run_route(hap, x, "f32", 7, sigmoid, True, groups=groups, best=2, seed=E)
