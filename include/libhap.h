@@ -419,7 +419,9 @@ int hap_reducescatter_split(const hap_gather_desc* d, const void* full, int64_t 
  * An expert whose logit or bias is -inf is never chosen; a choice that finds no expert has index -1 and weight 0 (a token all of whose
  * logits are -inf goes nowhere).  The order is that of the scores before rounding: without a bias the logits' own order, exactly;
  * scores plus bias, and sums over groups, are formed and compared in fp64.  NaN ranks
- * above every number; a NaN among the logits (or +inf under softmax) makes the token's weights NaN, its indices stay valid.
+ * above every number: where a softmax has no value (a NaN or +inf among the logits) the experts with such a logit come first, the others by
+ * their bias alone (without a bias by their logits), and the token's weights are NaN, even if a bias bars the expert.  With sigmoid scores a
+ * NaN logit makes that expert's weight NaN, and with renormalise all of the token's if it is chosen.  Indices are valid in any case.
  * tokens < 2^26, experts <= 1024, top_k <= 64, groups <= 64 (HAP_EUNSUPPORTED beyond); groups divides experts; top_k <= top_groups * experts / groups. */
 typedef enum { HAP_SCORE_SOFTMAX = 0, HAP_SCORE_SIGMOID = 1 } hap_score;
 typedef struct {
@@ -437,7 +439,8 @@ typedef struct {
 /* indices int32 [tokens x top_k], weights fp32 [tokens x top_k], both without gaps; bias fp32 [experts] or NULL. */
 int hap_moe_route_fwd(const hap_route_desc* d, const void* logits, const float* bias, int32_t* indices, float* weights, void* stream);
 /* dlogits from dweights (fp32 [tokens x top_k]), the choice held fixed: no gradient passes through bias, groups or order.  Choices
- * whose index is no expert (-1) add nothing, whatever their dweights; an index given twice adds twice.                              */
+ * whose index is no expert (-1) add nothing, whatever their dweights; an index given twice adds twice.  With renormalise, and with sigmoid
+ * scores, the chosen logits alone are read: what others hold does not matter.                                                     */
 int hap_moe_route_bwd(const hap_route_desc* d, const void* logits, const int32_t* indices, const float* dweights, void* dlogits, void* stream);
 
 /* The rows that the choices take in the experts' buffers (hap_moe_desc's X and `rows`): choice n = token * top_k + i takes

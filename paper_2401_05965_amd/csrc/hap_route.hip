@@ -187,8 +187,9 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
       double n = 0.0;
 #pragma unroll
       for (int r = 0; r < R; ++r) { rank[r] = exp((double)x[r] - (double)top); n += rank[r]; }
-      scale = 1.0 / sum<L>(n);
-      inv_total = (float)scale;
+      n = sum<L>(n);
+      scale = n == n ? 1.0 / n : 0.0;      // a NaN or +inf among the logits: their scores stay NaN, the others' are 0
+      inv_total = (float)(1.0 / n);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {          // (closed by either, whatever the score is: a NaN plus -inf is a NaN)
@@ -251,6 +252,7 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const RouteArgs a, const
     if (a.sigmoid) m = fminf(m, 0.0f);
     float s = chosen >= 0 ? (a.sigmoid ? (xi >= 0.0f ? 1.0f : expf(xi - m)) / (1.0f + expf(-fabsf(xi))) : expf(xi - m)) : 0.0f;
     w = s / sum<L>(s);
+    if (SUMS && inv_total != inv_total) w = inv_total;                // a softmax without a value, whoever was chosen (a bias can bar the culprit)
   }
   if (live && l < a.top_k) {
     indices[t * a.top_k + l] = chosen;

@@ -321,3 +321,68 @@ def test_route_order_inside_groups_over_layouts(hap, E):
     for groups in (2, E // 4, 8) if E < 200 else (2, 8, 32):
         for sigmoid in (False, True):
             run_route(hap, x, "f32", 7, sigmoid, True, groups=groups, best=2, seed=E)
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("E,groups,best,with_bias", [(8, 1, 1, False), (8, 1, 1, True), (30, 1, 1, True), (30, 5, 2, False), (30, 5, 2, True), (64, 8, 2, False), (256, 8, 2, True), (512, 1, 1, True),
+                                                     (900, 9, 2, False)])
+def test_route_bad_logits_far_from_the_first_experts_make_the_weights_nan(hap, bad, renorm, E, groups, best, with_bias):
+    """Softmax: an expert whose logit is NaN or +inf ranks first, wherever it lies; the token's weights and the gradients of what it chose are NaN; the other tokens do not notice."""
+    rng = np.random.default_rng(E)
+    k = 3
+    x = rng.normal(size=(5, E)).astype(np.float32)
+    bias = rng.permutation(E) / E - 0.5 if with_bias else None
+    x[1, E - 2] = bad
+    x[3, [E // 2, E - 1]] = bad
+    idx, w, dx = routed(hap, x, k, False, renorm, bias, groups, None, best)
+    assert idx[1, 0] == E - 2 and set(idx[3, :2]) == {E // 2, E - 1}
+    assert np.isnan(w[[1, 3]]).all()
+    for t in (1, 3):
+        assert np.isnan(dx[t][idx[t]]).all()
+    if with_bias:                                             # the others by their bias alone
+        for t, n in ((1, 1), (3, 2)):
+            rest = [e for e in np.argsort(-bias.astype(np.float32), kind="stable") if e not in set(idx[t, :n])]
+            assert idx[t, n:].tolist() == rest[:k - n]
+    else:                                                     # by their logits
+        rest = [e for e in np.argsort(-np.where(np.arange(E) == E - 2, -9e9, x[1]), kind="stable") if e != E - 2]
+        assert idx[1, 1:].tolist() == rest[:k - 1]
+    good = [0, 2, 4]
+    oi, ow = ort.route_fwd(x[good].astype(np.float64), k, False, bias.astype(np.float32).astype(np.float64) if with_bias else None, groups, None, best, renorm)
+    assert (idx[good] == oi).all() and (np.abs(w[good] - ow) <= 50 * U * np.abs(ow)).all() and np.isfinite(dx[good]).all()
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+def test_route_softmax_of_a_row_with_a_barred_bad_logit_has_no_value(hap, renorm):
+    """The softmax is one over all experts, the barred ones too: its weights are NaN, the choice goes by the bias."""
+    for E, groups, best in ((8, 1, 1), (30, 5, 2), (256, 8, 1)):
+        x = np.zeros((3, E), dtype=np.float32)
+        x[1, 2] = np.nan; x[2, 2] = np.inf
+        bias = -np.arange(E) / E; bias[2] = -np.inf
+        idx, w, _ = routed(hap, x, 4, False, renorm, bias, groups, None, best)
+        assert (idx == [0, 1, 3, 4]).all() and np.isfinite(w[0]).all() and np.isnan(w[1:]).all()
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("E,groups,best,with_bias", [(8, 1, 1, False), (30, 1, 1, True), (30, 5, 2, False), (256, 8, 2, True), (900, 9, 2, False)])
+def test_route_nan_under_sigmoid_scores_is_one_experts_own(hap, renorm, E, groups, best, with_bias):
+    """It ranks first; its own weight is NaN, and through the sum all of the token's where they are renormalised.  +inf is a score of 1."""
+    rng = np.random.default_rng(E)
+    k = 3
+    x = rng.normal(size=(4, E)).astype(np.float32)
+    bias = rng.permutation(E) / E - 0.5 if with_bias else None
+    x[1, E - 2] = np.nan
+    x[2, E - 2] = np.inf
+    idx, w, dx = routed(hap, x, k, True, renorm, bias, groups, None, best)
+    assert idx[1, 0] == E - 2 and np.isnan(w[1, 0])
+    b = bias.astype(np.float32).astype(np.float64) if with_bias else None
+    if renorm:
+        assert np.isnan(w[1]).all() and np.isnan(dx[1][idx[1]]).all()
+    else:
+        s = 1.0 / (1.0 + np.exp(-x[1][idx[1, 1:]].astype(np.float64)))
+        assert (np.abs(w[1, 1:] - s) <= 50 * U * s).all() and np.isnan(dx[1, E - 2])
+        assert np.isfinite(np.delete(dx[1], E - 2)).all()
+    big = x.astype(np.float64); big[2, E - 2] = 800.0         # (a score of 1 in 64 bits)
+    good = [0, 2, 3]
+    oi, ow = ort.route_fwd(big[good], k, True, b, groups, None, best, renorm)
+    assert (idx[good] == oi).all() and (np.abs(w[good] - ow) <= 50 * U * np.abs(ow)).all() and np.isfinite(dx[good]).all()
