@@ -150,11 +150,14 @@ __global__ __launch_bounds__(1024) void sumsq_final_kernel(int n, const double* 
 /* From the last tensor to the first (the table's order) and from a tensor's last item to its first: what the norm's pass read last is still in the last-level cache. */
 template <bool STREAM> __global__ __launch_bounds__(256) void clip_kernel(const Table a, const double* sumsq, double max_norm, float* norm) {
   const double total = *sumsq;
-  float factor = -1.0f;                // (not known yet: root and quotient are taken while the first chunks are on their way)
+  // The factor is mantissa * 2^power: as one fp32 number it would have few bits below 2^-126 (a norm of 1e36, clipped to 1e-3).  Not known yet: root and quotient
+  // are taken while the first chunks are on their way.
+  float mantissa = -1.0f;
+  int power = 0;
   const auto known = [&] {
-    if (factor < 0.0f) {
+    if (mantissa < 0.0f) {
       const double n = sqrt(total);
-      factor = n <= max_norm ? 1.0f : (float)(max_norm / n);       // (NaN for a NaN norm)
+      mantissa = n <= max_norm ? 1.0f : (float)frexp(max_norm / n, &power);       // (NaN for a NaN norm)
       if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     }
   };
@@ -163,7 +166,7 @@ template <bool STREAM> __global__ __launch_bounds__(256) void clip_kernel(const 
     const View t = view_of(a, which);
     if (t.g == t.out) {
       known();
-      if (factor == 1.0f) continue;    // in place and nothing to change
+      if (mantissa == 1.0f && power == 0) continue;    // in place and nothing to change
     }
     with_type_of(t, a.bf16[which], [&](auto type, auto width) {
       using T = decltype(type);
@@ -176,7 +179,7 @@ template <bool STREAM> __global__ __launch_bounds__(256) void clip_kernel(const 
         known();
         const int at = r * t.ldo + c;
 #pragma unroll
-        for (int v = 0; v < V; ++v) p.v[v] = (T)(to_f32(p.v[v]) * factor);
+        for (int v = 0; v < V; ++v) p.v[v] = (T)ldexpf(to_f32(p.v[v]) * mantissa, power);
         if (c >= lo && c + V <= hi) {
           if constexpr (STREAM && V > 1) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, p), reinterpret_cast<u32x4*>(out + at));
           else row_store<false>(to, at, p);

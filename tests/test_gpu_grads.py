@@ -141,3 +141,23 @@ def test_norms_that_are_no_numbers(hap):
         hap.hap_grad_sumsq(d, [g], total, ws)
         hap.hap_grad_clip(d, [g], [g], total, norm)
         assert torch.isnan(g[7]) and (torch.isnan(g).all() if math.isnan(bad) else ((g == 0).sum() == 99 and float(norm) == bad))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_factors_below_the_normal_range_of_fp32(hap, in_place):
+    """max_norm / norm of 1e-38 and less: the scaled values are ordinary numbers again."""
+    for max_norm in (1.0, 1e-3, 1e-6, 1e-12):
+        run_clip(hap, [(30, 40, 40, "f32", 0), (3, 100, 104, "bf16", 1), (1, 9, 9, "f32", 1)], max_norm, in_place, sigma=1e36)
+
+
+def test_a_norm_beyond_fp32_still_scales(hap):
+    """The norm itself is +inf in fp32; the factor is taken from the fp64 sum."""
+    torch = torch_mod()
+    g = torch.full((1 << 12,), 3e38, device="cuda"); g[1::2] = -1e38
+    d = hap.GradDesc([(1, 1 << 12, 1 << 12, hap.F32)], 1.0)
+    ws = torch.empty((hap.hap_grad_sumsq_workspace(d),), dtype=torch.uint8, device="cuda")
+    total = torch.empty((1,), dtype=torch.float64, device="cuda"); norm = torch.empty((1,), device="cuda"); out = torch.empty_like(g)
+    hap.hap_grad_sumsq(d, [g], total, ws)
+    hap.hap_grad_clip(d, [g], [out], total, norm)
+    want = g.double() / (g.double() ** 2).sum().sqrt()
+    assert float(norm) == math.inf and ((out.double() - want).abs() <= 3.03 * U * want.abs()).all()
