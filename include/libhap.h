@@ -447,7 +447,8 @@ int hap_moe_route_bwd(const hap_route_desc* d, const void* logits, const int32_t
  * position[n] = the number of lower n with the same expert, -1 if that is not below `capacity` (the choice is dropped) or its index is
  * not an expert (outside [0, experts)).  rows[e] = buffer rows of expert e that hold a token, as the expert layers take it;
  * counts[e] = choices of expert e, dropped ones included (NULL: not wanted).  All int32, indices and position [tokens x top_k] without
- * gaps.  tokens * top_k < 2^31, experts <= 1024, top_k <= 64.  ws from hap_moe_plan_workspace (0 for small batches).               */
+ * gaps.  tokens * top_k < 2^31, experts <= 1024, top_k <= 64.  ws from hap_moe_plan_workspace (0 for small batches),
+ * on a multiple of 4 bytes.                                                                                                         */
 int hap_moe_plan(int64_t tokens, int top_k, int64_t experts, int64_t capacity, const int32_t* indices, int32_t* position, int32_t* rows,
                  int32_t* counts, void* ws, size_t ws_bytes, void* stream);
 size_t hap_moe_plan_workspace(int64_t tokens, int top_k, int64_t experts);
@@ -503,7 +504,7 @@ typedef struct {
 int hap_embedding_fwd(const hap_embedding_desc* d, int shard_index, const void* ids, const void* W, void* Y, void* stream);
 /* dW[v] = scale * sum of dY[t] over the tokens with ids[t] = v, in fp32, rounded once; rows without a token get zeros.
  * accumulate = 1 adds the sums to dW's contents instead and leaves rows without a token alone.  dW like W, dW_dtype fp32 or (bf16
- * tables) bf16.  ws from hap_embedding_bwd_workspace.  The same bits in every run: no floating-point atomics.                     */
+ * tables) bf16.  ws from hap_embedding_bwd_workspace, on a multiple of 4 bytes.  The same bits in every run: no floating-point atomics. */
 int hap_embedding_bwd(const hap_embedding_desc* d, int shard_index, const void* ids, const void* dY, void* dW, int dW_dtype, int accumulate,
                       void* ws, size_t ws_bytes, void* stream);
 size_t hap_embedding_bwd_workspace(const hap_embedding_desc* d, int shard_index);
@@ -520,8 +521,8 @@ typedef struct {
 } hap_grad_desc;
 
 /* *sumsq (device, fp64) = sum of squares over all tensors, in fp64: the device's part of the squared norm, to be added up over the
- * devices (an All-Reduce of one number).  grads: HOST array of n device pointers.  ws from hap_grad_sumsq_workspace.  The same bits
- * in every run.                                                                                                                    */
+ * devices (an All-Reduce of one number).  grads: HOST array of n device pointers.  ws from hap_grad_sumsq_workspace, on a multiple of
+ * 8 bytes.  The same bits in every run.                                                                                           */
 int hap_grad_sumsq(const hap_grad_desc* d, const void* const* grads, double* sumsq, void* ws, size_t ws_bytes, void* stream);
 size_t hap_grad_sumsq_workspace(const hap_grad_desc* d);
 /* out_i = grads_i * min(1, max_norm / norm) with norm = sqrt(*sumsq), read on the device; *norm (device fp32, NULL: not wanted).

@@ -560,6 +560,7 @@ int hap_embedding_bwd(const hap_embedding_desc* d, int shard_index, const void* 
   if (!dW || (p.tokens > 0 && (!ids || !dY))) return hap_fail(HAP_EINVAL, "ids, dY or dW is NULL");
   const Plan q = plan_of(p);
   if (p.tokens > 0 && (!ws || ws_bytes < (size_t)q.bytes)) return hap_fail(HAP_EWORKSPACE, "embedding_bwd needs %lld workspace bytes", (long long)q.bytes);
+  if (p.tokens > 0 && (uintptr_t)ws % sizeof(uint32_t)) return hap_fail(HAP_EINVAL, "ws is not on a multiple of %zu bytes", sizeof(uint32_t));
   hipStream_t s = (hipStream_t)stream;
   const int es = esize(d->io_dtype), wes = esize(dW_dtype), V = 16 / wes;
   const char* y = static_cast<const char*>(dY) + y_offset(d, p) * es;

@@ -291,6 +291,7 @@ int hap_grad_sumsq(const hap_grad_desc* d, const void* const* grads, double* sum
     if (!grads[i] && d->rows[i] > 0 && d->cols[i] > 0) return hap_fail(HAP_EINVAL, "tensor %d is NULL", i);
   const size_t need = hap_grad_sumsq_workspace(d);
   if (!ws || ws_bytes < need) return hap_fail(HAP_EWORKSPACE, "grad_sumsq needs %zu workspace bytes", need);
+  if ((uintptr_t)ws % sizeof(double)) return hap_fail(HAP_EINVAL, "ws is not on a multiple of %zu bytes", sizeof(double));
   hipStream_t s = (hipStream_t)stream;
   double* part = static_cast<double*>(ws);
   int64_t parts = 0;                   // (at most kBlocks for each of the tables: the workspace's size)

@@ -376,6 +376,7 @@ int hap_moe_plan(int64_t tokens, int top_k, int64_t experts, int64_t capacity, c
   if (!rows || (tokens > 0 && (!indices || !position))) return hap_fail(HAP_EINVAL, "indices, position or rows is NULL");
   const size_t need = hap_moe_plan_workspace(tokens, top_k, experts);
   if (need && (!ws || ws_bytes < need)) return hap_fail(HAP_EWORKSPACE, "moe_plan needs %zu workspace bytes", need);
+  if (need && (uintptr_t)ws % sizeof(int)) return hap_fail(HAP_EINVAL, "ws is not on a multiple of %zu bytes", sizeof(int));
   const int64_t slots = tokens * top_k, blocks = plan_blocks(slots);
   const bool direct = slots <= kPlanDirect, ranges = slots > kPlanMost * kPlanRange;
   PlanArgs a = {slots, ranges ? (slots + blocks - 1) / blocks : kPlanRange, (int)experts, (int)capacity, 0, indices, position, rows, counts, direct ? NULL : static_cast<int*>(ws)};

@@ -215,3 +215,28 @@ def test_training_step_as_a_graph(hap):
             for n, (a, b) in enumerate(zip(outs, w)):
                 assert torch.equal(a, b), (rep, n)
             (torch.randn(300, 300, device="cuda") @ torch.randn(300, 300, device="cuda")).sum().item()
+
+
+def test_workspaces_on_odd_words(hap):
+    """Workspaces cut from a larger buffer one word behind a 256-byte boundary: the same bits as from its start."""
+    torch = torch_mod()
+    buf = torch.empty((1 << 23,), dtype=torch.uint8, device="cuda")
+    idx = torch.randint(-1, 30, (20_000, 3), dtype=torch.int32, device="cuda")
+    ids = torch.randint(-1, 500, (17_000,), device="cuda"); ids[:5000] = 7
+    dY = torch.randn(17_000, 40, device="cuda")
+    g = torch.randn(300, 500, device="cuda")
+    E = hap.EmbeddingDesc(17_000, 500, 40, hap.REPLICATED, None, hap.F32)
+    G = hap.GradDesc([(300, 500, 500, hap.F32)], 1.0)
+    need = [hap.hap_moe_plan_workspace(20_000, 3, 30), hap.hap_embedding_bwd_workspace(E, 0), hap.hap_grad_sumsq_workspace(G)]
+    assert min(need) > 0 and max(need) + 8 <= buf.numel()
+    got = []
+    for off in (0, 4):
+        pos, rows = torch.empty_like(idx), torch.empty((30,), dtype=torch.int32, device="cuda")
+        dW, total = torch.empty((500, 40), device="cuda"), torch.empty((1,), dtype=torch.float64, device="cuda")
+        buf.fill_(255); hap.hap_moe_plan(20_000, 3, 30, 1500, idx, pos, rows, None, buf[off:off + need[0]])
+        buf.fill_(255); hap.hap_embedding_bwd(E, 0, ids, dY, dW, hap.F32, ws=buf[off:off + need[1]])
+        buf.fill_(255); hap.hap_grad_sumsq(G, [g], total, buf[2 * off:2 * off + need[2]])
+        assert (buf[max(need) + 8:] == 255).all()
+        got.append((pos, rows, dW, total))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

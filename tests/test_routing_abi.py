@@ -155,3 +155,18 @@ def test_clipping_one_output_twice_is_refused(hap, n):
     d = hap.GradDesc(((2, 3, 3, hap.F32),) * n, 1.0)
     refused(hap, EINVAL, hap.hap_grad_clip, d, address, address, P)                          # a shared tensor that is listed twice
     refused(hap, EINVAL, hap.hap_grad_clip, d, [P * (i + 1000) for i in range(n)], address, P)
+
+
+def test_workspaces_off_their_words_are_refused(hap):
+    """Counts and keys are 32-bit words, partial sums of squares are doubles: a workspace cut from a larger buffer starts on a multiple of them."""
+    E = hap.EmbeddingDesc(9, 16, 16, hap.REPLICATED, None, hap.BF16)
+    G = hap.GradDesc(((2, 3, 3, hap.F32), (1, 5, 5, hap.F32)), 1.0)
+    need = [hap.hap_moe_plan_workspace(100_000, 2, 8), hap.hap_embedding_bwd_workspace(E, 0), hap.hap_grad_sumsq_workspace(G)]
+    two = (C.c_uint64 * 2)(P, P)
+    calls = [lambda ws, n: hap.lib.hap_moe_plan(100_000, 2, 8, 4, P, P, P, P, ws, n, 0), lambda ws, n: hap.lib.hap_embedding_bwd(C.byref(E.c), 0, P, P, P, hap.F32, 0, ws, n, 0),
+             lambda ws, n: hap.lib.hap_grad_sumsq(C.byref(G.c), two, P, ws, n, 0)]
+    for call, n, word in zip(calls, need, (4, 4, 8)):
+        assert n > 0
+        for off in range(1, word):
+            assert call(P + off, n) == EINVAL, (word, off)
+        assert call(P + 1, n - 1) == EWORKSPACE
