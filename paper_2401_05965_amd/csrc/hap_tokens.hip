@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void combine_fwd_kernel(const TokenArgs a, con
 }
 
 /* Two choices at a time, whose sums run through the whole row: dout is read again for the next two (from the caches). */
-template <typename T, int V, bool STREAM, bool CUT>
+template <typename T, int V, bool CUT>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(const TokenArgs a, const T* Y, const float* weights, const T* dout, T* dY, float* dweights) {
   constexpr int U = 2, STEP = 64 * V;
   const int lane = threadIdx.x & 63, bytes = chunk_bytes<T, V>(a.features);
@@ -274,8 +274,8 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(const TokenArgs a, con
           p[u].v[v] = (T)(wi * x);
           q[u].v[v] = (T)(wj * x);
         }
-        row_store_part<STREAM, CUT>(di, c + u * STEP, p[u], 0, a.features);      // (without dY, without a second choice: rows without bytes)
-        row_store_part<STREAM, CUT>(dj, c + u * STEP, q[u], 0, a.features);
+        row_store_part<false, CUT>(di, c + u * STEP, p[u], 0, a.features);      // (without dY, without a second choice: rows without bytes)
+        row_store_part<false, CUT>(dj, c + u * STEP, q[u], 0, a.features);
       }
     }
     si = sum<64>(si);
@@ -344,9 +344,11 @@ template <typename F> void with_type(int dtype, bool vec, F&& f) {
 
 inline dim3 token_grid(const TokenArgs& a) { return dim3((unsigned)((a.tokens + 3) / 4)); }
 
-/* Whether a launch that writes rows of the device's buffers stores non-temporally: where the choices can fill more than 300 MB (the last-level cache holds 256).
- * Write-through / non-temporal, alone and with the experts' product that reads the buffers: 268 MB 51.8 / 40.5 and 340 / 347 us, 537 MB 87.8 / 74.8
- * and 568 / 570. */
+/* Whether dispatch stores non-temporally: where the choices can fill more than 300 MB of the device's buffers (the last-level cache holds 256).  Write-through /
+ * non-temporal, alone and with the experts' product that reads the buffers (bf16, eight choices): 268 MB 60.5 / 53.0 and 354 / 358 us, 403 MB 89.0 / 76.7 and 502 / 496,
+ * 537 MB 117 / 102 and 631 / 628, 805 MB 181 / 154 and 984 / 983, 1074 MB 236 / 210 and 1249 / 1258; two choices, 537 MB 153 / 153 and 2150 / 2151: a gain of up to 15 % where
+ * the product does not follow at once (an exchange between devices comes first), and within its runs' spread where it does.  Combine's gradient gains nothing either way
+ * (403 MB 174 / 172 and 575 / 575, 1074 MB 459 / 455 and 1460 / 1461). */
 inline bool buffers_streamed(const TokenArgs& a, size_t es) {
   const int64_t rows = a.tokens * a.top_k < a.n * a.capacity ? a.tokens * a.top_k : a.n * a.capacity;
   return rows * a.features * (int64_t)es > (int64_t)300 << 20;
@@ -472,9 +474,7 @@ int hap_moe_combine_bwd(const hap_moe_tokens_desc* d, int shard_index, const voi
     using T = decltype(t);
     constexpr int V = decltype(v)::value;
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, token_grid(a), dim3(256), 0, (hipStream_t)stream, a, (const T*)Y, weights, (const T*)dout, (T*)dY, dweights); };
-    if (cut(a, V)) launch(combine_bwd_kernel<T, V, false, (V > 1)>);
-    else if (V > 1 && buffers_streamed(a, sizeof(T))) launch(combine_bwd_kernel<T, V, (V > 1), false>);
-    else launch(combine_bwd_kernel<T, V, false, false>);
+    if (cut(a, V)) launch(combine_bwd_kernel<T, V, (V > 1)>); else launch(combine_bwd_kernel<T, V, false>);
   });
   return check_launch("moe_combine_bwd");
 }

@@ -221,3 +221,37 @@ def test_buffers_beyond_two_to_the_31_elements(hap):
     dX = torch.empty_like(X)
     hap.hap_moe_combine_bwd(d, 0, X, idx, pos, 2 * w, x, dX, None)
     assert torch.equal(dX[2][pos[:, 0].long()], 2 * x)
+
+
+@pytest.mark.parametrize("dtype,h", [("bf16", 4096), ("f32", 2048)])
+def test_buffers_that_the_last_level_cache_does_not_hold(hap, dtype, h):
+    """340 MB of buffer rows, moved there and back: rows and gradients are exact, rows without a token stay as they were, an overflowing expert included."""
+    torch = torch_mod()
+    td = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    T, k, E, C = 5200, 8, 32, 1350
+    gen = torch.Generator(device="cuda"); gen.manual_seed(3)
+    score = torch.rand((T, E), device="cuda", generator=gen); score[:, 5] += 0.6; score[:, 6] -= 0.6
+    idx = score.argsort(dim=1, descending=True)[:, :k].int().contiguous()
+    idx[7] = -1
+    pos, rows = torch.empty_like(idx), torch.empty((E,), dtype=torch.int32, device="cuda")
+    ws = torch.empty((max(hap.hap_moe_plan_workspace(T, k, E), 16),), dtype=torch.uint8, device="cuda")
+    hap.hap_moe_plan(T, k, E, C, idx, pos, rows, None, ws)
+    live = pos >= 0
+    assert int(rows[5]) == C and int(rows.sum()) * h * (2 if dtype == "bf16" else 4) > 300 << 20
+    d = hap.MoeTokensDesc(T, k, E, C, h, [0, E], hap.BF16 if dtype == "bf16" else hap.F32)
+    x = torch.randint(-64, 65, (T, h), device="cuda", generator=gen).to(td)
+    X = torch.full((E, C, h), SENTINEL, dtype=td, device="cuda")
+    hap.hap_moe_dispatch_fwd(d, 0, x, idx, pos, X)
+    e, p, t = idx[live].long(), pos[live].long(), live.nonzero()[:, 0]
+    assert torch.equal(X[e, p], x[t])
+    empty = torch.arange(C, device="cuda")[None, :] >= rows[:, None]
+    assert (X[empty] == SENTINEL).all()
+    w = torch.randint(-2, 3, (T, k), device="cuda", generator=gen).float()
+    dX, dw, out = torch.full_like(X, SENTINEL), torch.empty_like(w), torch.empty_like(x)
+    hap.hap_moe_combine_bwd(d, 0, X, idx, pos, w, x, dX, dw)
+    assert torch.equal(dX[e, p], x[t] * w[live][:, None].to(td)) and (dX[empty] == SENTINEL).all()
+    # whole numbers: sums below 2^24 are exact in fp32 whatever their order
+    norm = (x.double() ** 2).sum(dim=1)
+    assert torch.equal(dw.double(), torch.where(live, norm[:, None], torch.zeros_like(norm)[:, None]))
+    hap.hap_moe_combine_fwd(d, 0, X, idx, pos, w, out)
+    assert torch.equal(out, (x.double() * torch.where(live, w, torch.zeros_like(w)).double().sum(dim=1)[:, None]).to(td))
