@@ -528,9 +528,10 @@ int hap_embedding_fwd(const hap_embedding_desc* d, int shard_index, const void* 
   with_type(d->io_dtype, vec, [&](auto t, auto v) {
     using T = decltype(t);
     constexpr int N = decltype(v)::value;
-    // Non-temporal stores from 80 MB on.  Write-through / non-temporal, with a pass that reads the result (bf16 rows of 2048 and of 5120): 56 MB 35.7 / 37.6 and
-    // 37.5 / 41.1 us, 72 MB 46.2 / 46.8 and 48.8 / 51.1, 88 MB 60.6 / 55.8 and 64.1 / 61.2, 104 MB 72.9 / 67.1 and 77.0 / 73.7, 152 MB 105 / 106 and 111 / 115,
-    // 200 MB 136 / 135 and 143 / 146; alone non-temporal takes less at every size (72 MB 23.5 / 22.1 and 27.1 / 23.9, 200 MB 60.2 / 58.2 and 72.2 / 60.0).
+    // Non-temporal stores from 80 MB on.  Write-through / non-temporal with a pass behind that reads the result and writes as much, bf16 rows of 2048 and of 5120, us:
+    // 56 MB 36.1 / 37.9 and 37.5 / 40.6, 72 MB 45.6 / 46.5 and 49.0 / 51.4, 88 MB 59.3 / 56.0 and 63.2 / 61.4, 104 MB 73.0 / 67.2 and 76.7 / 73.6, 152 MB 106 / 106 and
+    // 111 / 115, 256 MB 170 / 168 and 181 / 186, 400 MB 257 / 250 and 277 / 277, 800 MB 495 / 480 and 540 / 520: -8 to +3.4 % from 88 MB on, -1.4 % in the mean (wide rows
+    // of 128 to 320 MB are those that lose).  Without a reader at once it takes less at every size (88 MB 27.9 / 26.5 and 33.2 / 29.6, 256 MB 76.2 / 73.9 and 92.0 / 76.7).
     const auto launch = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((p.tokens + 3) / 4)), dim3(256), 0, (hipStream_t)stream, p.tokens, vec ? first : 0, (int)p.cols + (vec ? first : 0), i, reinterpret_cast<const T*>(w), d->ldw, d->scale,
                          reinterpret_cast<T*>(y), d->ldy);

@@ -208,3 +208,26 @@ def test_tables_beyond_two_to_the_31_elements(hap):
     hap.hap_embedding_bwd(d, 0, ids, Y, dW, hap.BF16, ws=ws)
     assert torch.equal(dW[V - 1], (Y[0].float() + Y[4].float()).bfloat16()) and torch.equal(dW[524_288], Y[3]) and torch.equal(dW[V - 2], Y[2])
     assert (dW[V // 2] == 0).all() and (dW[V - 5:V - 2] == 0).all() and int((dW != 0).any(dim=1).sum()) == 5
+
+
+@pytest.mark.parametrize("dtype,h", [("bf16", 5120), ("f32", 2048)])
+def test_lookups_that_the_caches_do_not_hold(hap, dtype, h):
+    """90 MB of looked-up rows: the table's rows times a power of two exactly, zeros for padding; whole rows and columns that begin inside a chunk."""
+    torch = torch_mod()
+    td = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    V = 3001
+    T = 90_000_000 // (h * (2 if dtype == "bf16" else 4)) + 1
+    gen = torch.Generator(device="cuda"); gen.manual_seed(h)
+    W = torch.randn((V, h), device="cuda", generator=gen).to(td)
+    ids = torch.randint(-50, V + 50, (T,), device="cuda", generator=gen)
+    here = (ids >= 0) & (ids < V)
+    want = torch.where(here[:, None], 2 * W[ids.clamp(0, V - 1)], torch.zeros((), dtype=td, device="cuda"))
+    io = hap.BF16 if dtype == "bf16" else hap.F32
+    Y = torch.full((T, h), SENTINEL, dtype=td, device="cuda")
+    hap.hap_embedding_fwd(hap.EmbeddingDesc(T, V, h, hap.REPLICATED, None, io, scale=2.0), 0, ids, W, Y)
+    assert torch.equal(Y, want)
+    Y.fill_(SENTINEL)
+    d = hap.EmbeddingDesc(T, V, h, hap.SHARD_FEATURE, [0, 8, h - 3, h], io, scale=2.0)
+    for j in range(3):
+        hap.hap_embedding_fwd(d, j, ids, W, Y)
+    assert torch.equal(Y, want)
