@@ -6,7 +6,8 @@
  *
  * Bound: HBM; the gradient's largest part is usually the table itself, written whole.  Its steps:
  *   1  sort the tokens by id (stable counting sort by digits, hap_sort.h); up to kSortAlone tokens one workgroup does it while the other
- *      workgroups of the launch fill the table with zeros, so that the sort costs nothing beside a table of any size
+ *      workgroups of the launch fill the table with zeros.  The sort costs nothing where the fill takes longer: 8192 tokens 19 us, a fill of 125 MB;
+ *      16384 tokens 27 us, 180 MB.  A smaller table, and an accumulating pass, which fills nothing, wait for it
  *   2  chunks of the sorted tokens, one wave per chunk and 64 vectors of columns: rows of one id follow each other and are summed in registers;
  *      an id whose tokens all lie in the chunk is finished and stored, one that crosses the chunk's borders leaves a partial row
  *   3  the partial rows of an id are added up by the workgroup of the chunk in which it begins
@@ -139,9 +140,18 @@ __device__ __forceinline__ void sort_pass(const SortArgs& a, int pass, int b, in
   with_entries(a, pass, [&](auto load, auto digit_of, auto place) { hap_sort::place_keys(count, values, a.bits, begin, end, load, digit_of, place); });
 }
 
-/* Non-temporal up to 128 MB: the sums that follow then find room in the last-level cache.  Plain / non-temporal, lookup and gradient, and with a pass that reads the
- * whole gradient behind them: 63 MB 49.6 / 43.0 and 68.9 / 70.0 us, 125 MB 50.2 / 41.6 and 76.2 / 74.7, 206 MB 61.1 / 61.0 and 96.5 / 111.6, 437 MB 173 / 176
- * and 299 / 296. */
+/* Non-temporal as long as the one workgroup's sort beside it takes longer or about as long: little waits for the stores then, and the sums that follow find room in the
+ * last-level cache.  That is up to 50 MB and 11 KB more for every token (fill_streamed).  Plain / non-temporal, three sets of buffers in turn, gradient alone and with the norm
+ * over it behind, which reads all of it, us:
+ *   300 tokens of 1024      30 MB 17.7 / 16.9 and 27.5 / 27.1     63 MB 18.6 / 18.2 and 32.8 / 35.2    125 MB 29.6 / 29.9 and 50.7 / 56.3
+ *   2000 of 4096            63 MB 27.4 / 25.5 and 41.6 / 40.8     94 MB 34.3 / 29.2 and 53.9 / 53.1    125 MB 35.3 / 34.6 and 59.3 / 63.1
+ *   4096 of 2560, bf16      94 MB 38.7 / 30.5 and 59.4 / 58.1    110 MB 39.1 / 33.9 and 61.9 / 62.7    156 MB 43.4 / 42.2 and 71.5 / 78.7
+ *   8192 of 1024           125 MB 44.5 / 36.5 and 68.0 / 67.3    140 MB 44.7 / 40.2 and 70.4 / 71.0    156 MB 44.7 / 43.6 and 73.1 / 78.1
+ *   8192 of 4096, bf16     125 MB 59.7 / 57.8 and 84.7 / 82.9    156 MB 59.4 / 61.2 and 94.5 / 92.0    200 MB 69.8 / 71.1 and 100.5 / 110.1
+ *   16384 of 768           140 MB 60.7 / 51.0 and 86.0 / 85.6    200 MB 60.4 / 56.7 and 96.6 / 98.6    250 MB 66.8 / 65.6 and 105.0 / 116.9
+ *   16384 of 4096, bf16    156 MB 99.6 / 93.3 and 125 / 117      200 MB 105 / 95 and 136 / 128         320 MB 118 / 122 and 180 / 181
+ * (two sets, which the cache half holds: 8192 of 1024, 125 MB 35.6 / 34.9 and 59.3 / 61.6).  Many workgroups' sort is too short: 32768 of 2048, 63 MB 93.5 / 96.0 and
+ * 110 / 111, 200 MB 135 / 143 and 169 / 172. */
 struct FillArgs {
   char* p;
   int64_t rows, ld;                    // ld in bytes
@@ -482,6 +492,8 @@ template <typename F> void with_type(int dtype, bool vec, F&& f) {
   }
 }
 
+inline bool fill_streamed(const Plan& q, int64_t tokens, int64_t bytes) { return q.alone && bytes <= 50'000'000 + 11'000 * tokens; }
+
 /* Fills the device's part of the table with zeros and sorts; *sorted: which of the two buffers holds the result. */
 int sort_tokens(const SortArgs& a, const Plan& q, const FillArgs& f, int* sorted, hipStream_t s) {
   const size_t lds = (size_t)hap_sort::kWaves * sizeof(int) << q.bits, row = sizeof(int) << q.bits;
@@ -571,7 +583,7 @@ int hap_embedding_bwd(const hap_embedding_desc* d, int shard_index, const void* 
   if (!grid_fits(waves)) return hap_fail(HAP_EUNSUPPORTED, "%lld chunks of 64 tokens and %d columns, 2^24 and more", (long long)waves, slab);
   const int64_t pitch = d->ldw * wes, width = p.cols * wes;
   const uintptr_t phase = (uintptr_t)w | (uintptr_t)pitch | (uintptr_t)width;
-  const FillArgs f = {w, accumulate ? 0 : p.rows, pitch, (int)width, phase % 4 == 0 ? 4 : 2, p.rows * width <= (int64_t)128 << 20};
+  const FillArgs f = {w, accumulate ? 0 : p.rows, pitch, (int)width, phase % 4 == 0 ? 4 : 2, fill_streamed(q, p.tokens, p.rows * width)};
   char* const b = static_cast<char*>(ws);
   SortArgs a = {p.tokens, (p.tokens + q.blocks - 1) / q.blocks, ids_of(d, p, ids), q.passes, q.bits, {}, {}, NULL};
   for (int i = 0; i < 2; ++i) {
