@@ -322,7 +322,9 @@ int hap_grad_clip(const hap_grad_desc* d, const void* const* grads, void* const*
   hipStream_t s = (hipStream_t)stream;
   int64_t bytes = 0;
   for (int i = 0; i < d->n; ++i) bytes += d->rows[i] * d->cols[i] * (d->dtype[i] == HAP_BF16 ? 2 : 4);
-  const bool stream_out = bytes > (int64_t)256 << 20;        // (more than the last-level cache holds: 1.14 GB 532 -> 444 us)
+  // More than the last-level cache holds.  Norm and clipping, fp32, written through / non-temporally, alone and with a pass that reads the result: 260 MB 160 / 132 and
+  // 304 / 289 us, 400 MB 241 / 213 and 457 / 446, 1100 MB 651 / 618 and 1229 / 1208.
+  const bool stream_out = bytes > (int64_t)256 << 20;
   Table a;
   bool any = false;
   for (int next = d->n - 1; next_batch(d, grads, out, ldo, -1, &next, &a); any = true) {

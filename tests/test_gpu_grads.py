@@ -161,3 +161,43 @@ def test_a_norm_beyond_fp32_still_scales(hap):
     hap.hap_grad_clip(d, [g], [out], total, norm)
     want = g.double() / (g.double() ** 2).sum().sqrt()
     assert float(norm) == math.inf and ((out.double() - want).abs() <= 3.03 * U * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_that_the_last_level_cache_does_not_hold(hap, dtype):
+    """280 MB of gradients, scaled into other buffers and in place: whole tensors, rows in a pitch, views that begin and end inside a chunk; what lies around them stays."""
+    torch = torch_mod()
+    td, io, es = {"bf16": (torch.bfloat16, hap.BF16, 2), "f32": (torch.float32, hap.F32, 4)}[dtype]
+    gen = torch.Generator(device="cuda"); gen.manual_seed(8)
+    n = 280_000_000 // es
+    shapes = [(1, n // 2 + 5, n // 2 + 5, 3), (999, 4091, 4096, 0), (n // 2 // 2048, 2048, 2048, 0), (1, 8193, 8193, 7)]
+    bufs = [torch.empty((s + r * ld + 11,), dtype=td, device="cuda").normal_(0, 1, generator=gen) for r, _, ld, s in shapes]
+    cut = lambda bs: [b[s:s + r * ld].view(r, ld)[:, :c] for b, (r, c, ld, s) in zip(bs, shapes)]
+    g = cut(bufs)
+    assert sum(t.numel() for t in g) * es > 256 << 20
+    d = hap.GradDesc([(r, c, ld, io) for r, c, ld, _ in shapes], 0.75)
+    ws = torch.empty((hap.hap_grad_sumsq_workspace(d),), dtype=torch.uint8, device="cuda")
+    total, norm = torch.empty((1,), dtype=torch.float64, device="cuda"), torch.empty((1,), device="cuda")
+    hap.hap_grad_sumsq(d, g, total, ws)
+    want = sum(float((t.double() ** 2).sum()) for t in g)
+    assert float(total) == pytest.approx(want, rel=1e-12)
+    factor = 0.75 / math.sqrt(want)
+    obufs = [torch.full_like(b, SENTINEL) for b in bufs]
+    outs = cut(obufs)
+    hap.hap_grad_clip(d, g, outs, total, norm)
+    assert float(norm) == pytest.approx(math.sqrt(want), rel=1.01 * U)
+    for t, o in zip(g, outs):
+        ref = t.double() * factor
+        assert ((o.double() - ref).abs() <= 1.01 * (HALF[dtype] + 2 * U) * ref.abs()).all()
+    for o in outs:
+        o.fill_(SENTINEL)
+    # nothing outside of the views was written
+    assert all((b == SENTINEL).all() for b in obufs)
+    hap.hap_grad_clip(d, g, outs, total)
+    before = [b.clone() for b in bufs]
+    hap.hap_grad_clip(d, g, g, total)
+    for a, b in zip(g, outs):
+        assert torch.equal(a, b)
+    for t, b in zip(cut(before), g):
+        t.copy_(b)
+    assert all(torch.equal(a, b) for a, b in zip(before, bufs))
