@@ -368,8 +368,8 @@ int resolve(const hap_route_desc* d, RouteArgs* a) {
   return HAP_OK;
 }
 
-/* f(lanes per token, experts per lane): lanes for the choices and the groups.  Sixteen lanes with sixteen experts each beat 32 with eight (8192 / 65536 tokens, 8 of 256 in
- * groups: 12.2 / 61.6 us against 13.3 / 75.0) and one per lane for 64 (8 of 512: 33 / 223 with 64 x 16, 20 / 142 with 64 x 8). */
+/* f(lanes per token, experts per lane): lanes for the choices and the groups, many experts each.  With a bias, 8192 / 65536 tokens: 8 of 256 in groups 11.8 / 57.6 us with 16 x 16
+ * and 12.2 / 69.4 with 32 x 8; 8 of 512 16.2 / 98.4 with 32 x 16 and 17.8 / 117.7 with 64 x 8; 8 of 64 19.3 with 16 x 4 and 50.1 with 64 x 1 (65536). */
 template <typename F> void with_layout(const RouteArgs& a, F&& f) {
   const int lanes = a.top_k > a.groups ? a.top_k : a.groups;
 #define HAP_LAYOUT(L, R) f(std::integral_constant<int, L>(), std::integral_constant<int, R>())

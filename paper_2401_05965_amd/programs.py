@@ -190,7 +190,8 @@ class MoeLayerShard:
 
     Tokens, router and plan are whole on every device (the replicated rule); the expert axis is sharded, so that the device's `y`
     is a partial sum (to All-Reduce), and so are its `dx` and the router's `dWr`: the router's gradient is linear in the weights' gradients,
-    of which the device has those of its own experts.  `balance` (fp32 [experts] or None) is the bias that takes part in the choice only;
+    of which the device has those of its own experts.  The logits are rounded to the layer's type, as the linear layers store all results: bf16 tokens are
+    routed by bf16 logits, in the forward and in the gradient alike (fp32 ones of a caller's own go to hap_moe_route_* directly).  `balance` (fp32 [experts] or None) is the bias that takes part in the choice only;
     `counts` holds what a balancing rule updates it from.
     """
 
